@@ -34,6 +34,9 @@ extern "C" {
 /* Elements that share a scale byte in Q8. */
 #define MXQ_Q8_BLOCK 32
 
+/* How mxq_linear may hold its sums. */
+enum mxq_sums { MXQ_SUMS_F32 = 0, MXQ_SUMS_MX = 1 };
+
 /* Longest row of mxq_add_rmsnorm and its backward pass. */
 #define MXQ_NORM_MAX_COLS 16384
 
@@ -115,9 +118,10 @@ MXQ_API int mxq_swiglu_backward(const void* dh, int64_t ld_dh, const uint8_t* ga
  * X the activations (m x k, bf16 or Q8), W[j, l] = q * S the packed weights (n x k), T their
  * per-tensor scale.  W is never unpacked in memory.  Products of elements are exact (bf16 holds q * S and
  * Q8's elements), sums are fp32, y is rounded once; the adapters' inner product enters the second one as
- * two bf16 parts (16 bits).  Q8 against E8M0 weights of block 32 and more, with a bf16 output, multiplies
- * in the formats themselves: the scaled matrix instruction sums 128 products with an error of up to
- * 2^-14 of their magnitudes (2^-18 where their sizes are alike) before it adds them in fp32.
+ * two bf16 parts (16 bits).  With MXQ_SUMS_MX, Q8 against E8M0 weights of block 32 and more, with a bf16
+ * output, multiplies in the formats themselves, up to twice as fast: the scaled matrix instruction sums 128
+ * products with an error of up to 2^-14 of their magnitudes (2^-18 where their sizes are alike) before it
+ * adds them in fp32.
  *
  *   x, ld_x       device, m x k bf16, rows 16-byte aligned; NULL if x_codes is given
  *   x_codes, x_scales   device, m x k as Q8, 16-byte and 1-byte aligned; NULL if x is given
@@ -133,6 +137,8 @@ MXQ_API int mxq_swiglu_backward(const void* dh, int64_t ld_dh, const uint8_t* ga
  *   adapter_ids   device, m int32: the adapter of each row.  A value outside 0 .. adapter_count-1 means
  *                 none.  NULL: every row takes adapter 0
  *   adapter_rank  8 .. 64, a multiple of 8
+ *   sums          MXQ_SUMS_F32, or MXQ_SUMS_MX: the caller takes the sums of the scaled matrix instruction where
+ *                 types, format and block allow it (elsewhere as MXQ_SUMS_F32)
  *   y, ld_y       device, m x n of y_dtype, row stride ld_y >= n, aligned to its elements; not
  *                 overlapping an input
  *   workspace     device, 16-byte aligned, at least mxq_linear_workspace_size(args) bytes (often 0); contents need
@@ -161,6 +167,7 @@ typedef struct mxq_linear_args {
     int y_dtype;
     void* workspace;
     size_t workspace_bytes;
+    int sums;
 } mxq_linear_args;
 MXQ_API size_t mxq_linear_workspace_size(const mxq_linear_args* args);
 MXQ_API int mxq_linear(const mxq_linear_args* args, void* stream);

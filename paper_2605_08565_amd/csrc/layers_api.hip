@@ -48,7 +48,7 @@ mxq::LinearArgs linear_of(const mxq_linear_args& g)
     return {g.x, g.ld_x, g.x_codes, g.x_scales, (int)g.m, (int)g.n, (int)g.k, g.w_codes, g.w_scales, g.block, g.scale_fmt,
             g.tensor_scale, g.tensor_scale_dev, static_cast<const uint16_t*>(g.adapter_a), static_cast<const uint16_t*>(g.adapter_b),
             g.adapter_scaling, g.adapter_ids, adapters ? g.adapter_count : 0, adapters ? g.adapter_rank : 0, g.y, g.ld_y, g.y_dtype,
-            nullptr, 0, 0, 0, nullptr, 1, 0};
+            g.sums == MXQ_SUMS_MX, nullptr, 0, 0, 0, nullptr, 1, 0};
 }
 
 // Everything that the sizes of workspace and launch depend on.
@@ -59,6 +59,7 @@ int check_linear(const mxq_linear_args& g)
     if (g.k % MXQ_Q8_BLOCK != 0 || g.k % g.block != 0) return MXQ_ERR_INVALID_ARG;
     if (g.scale_fmt < MXQ_SCALE_E8M0 || g.scale_fmt > MXQ_SCALE_UE5M3) return MXQ_ERR_INVALID_ARG;
     if (g.y_dtype != MXQ_DT_BF16 && g.y_dtype != MXQ_DT_F32) return MXQ_ERR_INVALID_ARG;
+    if (g.sums != MXQ_SUMS_F32 && g.sums != MXQ_SUMS_MX) return MXQ_ERR_INVALID_ARG;
     if ((g.adapter_a == nullptr) != (g.adapter_b == nullptr)) return MXQ_ERR_INVALID_ARG;
     if (g.adapter_a) {
         if (!g.adapter_scaling || g.adapter_count < 1) return MXQ_ERR_INVALID_ARG;

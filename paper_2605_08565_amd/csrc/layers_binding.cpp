@@ -245,12 +245,13 @@ PyObject* swiglu_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// linear(x, w, adapters, ids, out_dtype), the output made here
+// linear(x, w, adapters, ids, out_dtype, sums), the output made here
 PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 5 || modes_active() || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 5 || !THPDtype_Check(a[4])) return none();
+    if (n != 6 || modes_active() || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 5 || !THPDtype_Check(a[4])) return none();
     mxq_linear_args g = {};
+    if (!integer(a[5], 0, 255, &g.sums)) return none();
     const at::Tensor* x = nullptr;
     Bits bits;
     if (PyTuple_Check(a[0])) {

@@ -835,11 +835,11 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(LinearArgs a)
 }
 
 // Whether Q8 and the weights multiply as they are.  The scaled matrix instruction sums its 128 products with about 21 bits of the
-// largest (error against 64 bits, 2-norm: 4.2e-6, fp32 sums of widened elements 3e-7), which a bf16 output does not show
-// (1.7e-3) and an fp32 output does: that one is widened.
+// largest (error against 64 bits, 2-norm: 4.2e-6, fp32 sums of widened elements 3e-7): a bf16 output (1.7e-3) shows that where its terms
+// cancel, so it is the caller's choice; an fp32 output would show it everywhere and is widened.
 bool scaled_products(const LinearArgs& a)
 {
-    return a.x_codes && a.scale_fmt == kE8M0 && a.block >= 32 && a.y_dtype == kBF16;
+    return a.mx_sums && a.x_codes && a.scale_fmt == kE8M0 && a.block >= 32 && a.y_dtype == kBF16;
 }
 
 LinearPlan plan_of(const LinearArgs& a) { return plan_linear({a.m, a.n, a.k, a.block, a.x != nullptr, scaled_products(a), a.rank}); }

@@ -79,6 +79,7 @@ struct LinearArgs {
     void* y;
     int64_t ld_y;
     int y_dtype;
+    bool mx_sums;              // the scaled instruction's sums will do
     // set by the launch
     float* low;                // low_parts x m x rank: scaling * x * A^T, in parts of k to be added up
     int low_parts, low_slots;  // low_slots: different adapters that 16 rows can have

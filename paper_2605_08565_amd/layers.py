@@ -21,6 +21,7 @@ from . import mxq
 from .mxq import _check, _done, _dtype_code, _need, _stream_ptr
 
 Q8_BLOCK = 32
+SUMS_F32, SUMS_MX = 0, 1                # how linear may hold its sums
 
 
 class Q8(NamedTuple):
@@ -71,7 +72,7 @@ class _Linear(ctypes.Structure):
                 ("adapter_a", ctypes.c_void_p), ("adapter_b", ctypes.c_void_p), ("adapter_scaling", ctypes.c_void_p),
                 ("adapter_ids", ctypes.c_void_p), ("adapter_count", ctypes.c_int), ("adapter_rank", ctypes.c_int),
                 ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("y_dtype", ctypes.c_int),
-                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("sums", ctypes.c_int)]
 
 
 _lib = None
@@ -278,12 +279,14 @@ def swiglu_backward(dh: torch.Tensor, saved: SavedSwiglu, again: bool = False, s
 
 
 def linear(x, w: W4, adapters: Adapters | None = None, ids: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
-           out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+           out: torch.Tensor | None = None, stream=None, sums: int = SUMS_F32) -> torch.Tensor:
     """mxq_linear: y = x W^T over packed FP4 weights, plus the low-rank adapter of each row.  x is Q8 or a bfloat16 tensor with
     contiguous rows; ids (int32, one a row) says which adapter a row has, values outside of 0 .. count-1 that it has none, and may
-    be left out when there is one adapter for all.  y is bfloat16 or float32; `out` may have any row stride."""
+    be left out when there is one adapter for all.  y is bfloat16 or float32; `out` may have any row stride.  Sums are held in 32
+    bits; SUMS_MX takes about 21 bits within each 128 of k for twice the rate, where x is Q8, y bfloat16 and the weights have E8M0
+    scales of 32 elements or more."""
     if _calls is not None and stream is None and out is None:
-        done = _calls.linear(x, w, adapters, ids, out_dtype)
+        done = _calls.linear(x, w, adapters, ids, out_dtype, sums)
         if done is not None:
             return _done(done)
     codes, scales, block, scale_fmt, tensor_scale = w
@@ -302,7 +305,8 @@ def linear(x, w: W4, adapters: Adapters | None = None, ids: torch.Tensor | None 
     if block <= 0:
         raise ValueError("block must be positive")
     _whole(scales, "w scales", (n, k // block), torch.uint8, dev)
-    args = _Linear(m=m, n=n, k=k, w_codes=codes.data_ptr(), w_scales=scales.data_ptr(), block=block, scale_fmt=scale_fmt)
+    args = _Linear(m=m, n=n, k=k, w_codes=codes.data_ptr(), w_scales=scales.data_ptr(), block=block, scale_fmt=scale_fmt,
+                   sums=sums)
     if isinstance(x, torch.Tensor):
         args.x, args.ld_x = x.data_ptr(), x.stride(0)
     else:

@@ -4,7 +4,7 @@ Serving (``MLP.serve``): norm with the residual's addition -> gate and up in one
 activations between them in 8 bits, the weights in packed FP4, every row with its request's low-rank adapters.
 Training (``train_block``): the same block with dense products; what norm and activation keep for the backward pass is in 8 bits.
 
-    python -m paper_2605_08565_amd.mlp [--hidden 4096] [--mlp 14336] [--adapters 8] [--tokens 1,16,512] [--train 2048]
+    python -m paper_2605_08565_amd.mlp [--hidden 4096] [--mlp 14336] [--adapters 8] [--tokens 1,16,512] [--train 2048] [--mx-sums]
 
 Prints one JSON line: times, the serving path's distance from the block in fp32, and what training keeps and how far its gradients are.
 """
@@ -21,8 +21,8 @@ from .layers import Adapters, Q8, SavedNorm, SavedSwiglu, W4
 
 
 def pack(weight: torch.Tensor, block: int = 32, scale_fmt: int = mxq.SCALE_E8M0, recipe: int = mxq.RECIPE_ABSMAX) -> W4:
-    """Dense weights [n, k] as linear takes them.  Power-of-two scales of 32 multiply with 8-bit activations as they are; E4M3 scales
-    of 16 (with RECIPE_4OVER6) are closer to the weights and are widened on the way."""
+    """Dense weights [n, k] as linear takes them.  Power-of-two scales of 32 can multiply with 8-bit activations as they are
+    (layers.SUMS_MX); E4M3 scales of 16 (with RECIPE_4OVER6) are closer to the weights."""
     if scale_fmt == mxq.SCALE_E8M0:
         codes, scales, _ = mxq.quantize(weight, block, scale_fmt, recipe, want_sse=False)
         return W4(codes, scales, block, scale_fmt)
@@ -31,11 +31,12 @@ def pack(weight: torch.Tensor, block: int = 32, scale_fmt: int = mxq.SCALE_E8M0,
 
 
 class MLP:
-    """A served block: packed weights and the adapters of its two projections (or None)."""
+    """A served block: packed weights and the adapters of its two projections (or None).  `sums`: how the projections hold their
+    sums (layers.linear)."""
 
     def __init__(self, norm_weight: torch.Tensor, gate_up: W4, down: W4, adapters_gate_up: Adapters | None = None,
-                 adapters_down: Adapters | None = None, eps: float = 1e-5):
-        self.norm_weight, self.gate_up, self.down, self.eps = norm_weight, gate_up, down, eps
+                 adapters_down: Adapters | None = None, eps: float = 1e-5, sums: int = layers.SUMS_F32):
+        self.norm_weight, self.gate_up, self.down, self.eps, self.sums = norm_weight, gate_up, down, eps, sums
         self.adapters_gate_up, self.adapters_down = adapters_gate_up, adapters_down
         self.width = gate_up.codes.shape[0] // 2
 
@@ -43,9 +44,9 @@ class MLP:
         """(the block's output, the updated residual stream): x and residual [tokens, hidden], ids the adapter of each token.  The
         residual is updated in place."""
         y, hidden, _ = layers.add_rmsnorm(x, self.norm_weight, residual, self.eps, hidden_out=residual)
-        both = layers.linear(y, self.gate_up, self.adapters_gate_up, ids if self.adapters_gate_up is not None else None)
+        both = layers.linear(y, self.gate_up, self.adapters_gate_up, ids if self.adapters_gate_up is not None else None, sums=self.sums)
         h, _ = layers.swiglu(both[:, :self.width], both[:, self.width:])
-        return layers.linear(h, self.down, self.adapters_down, ids if self.adapters_down is not None else None), hidden
+        return layers.linear(h, self.down, self.adapters_down, ids if self.adapters_down is not None else None, sums=self.sums), hidden
 
 
 class AddRMSNorm(torch.autograd.Function):
@@ -128,11 +129,12 @@ def _timed(f, reps=50):
     return (time.perf_counter() - began) / reps * 1e6
 
 
-def run(hidden: int, width: int, count: int, tokens, train: int) -> dict:
+def run(hidden: int, width: int, count: int, tokens, train: int, sums: int = layers.SUMS_F32) -> dict:
     out = {"hidden": hidden, "mlp": width, "adapters": count, "serve": {}}
     gen = torch.Generator(device="cuda")
     gen.manual_seed(7)
     block, back = make(hidden, width, count)
+    block.sums = sums
     for m in tokens:
         x, residual = _random(gen, m, hidden), _random(gen, m, hidden)
         ids = torch.randint(0, max(count, 1), (m,), generator=gen, device="cuda", dtype=torch.int32) if count else None
@@ -167,8 +169,10 @@ def main() -> None:
     ap.add_argument("--adapters", type=int, default=8)
     ap.add_argument("--tokens", default="1,16,512")
     ap.add_argument("--train", type=int, default=2048)
+    ap.add_argument("--mx-sums", action="store_true", help="sums of the scaled matrix instruction: about 21 bits, up to twice as fast")
     a = ap.parse_args()
-    print(json.dumps(run(a.hidden, a.mlp, a.adapters, [int(t) for t in a.tokens.split(",")], a.train)), flush=True)
+    print(json.dumps(run(a.hidden, a.mlp, a.adapters, [int(t) for t in a.tokens.split(",")], a.train,
+                         layers.SUMS_MX if a.mx_sums else layers.SUMS_F32)), flush=True)
 
 
 if __name__ == "__main__":
