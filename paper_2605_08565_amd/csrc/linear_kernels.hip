@@ -64,12 +64,11 @@ __device__ __forceinline__ uint4 buffer_load16(__amdgpu_buffer_rsrc_t b, uint32_
 {
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, scalar, 0));
 }
-// Scale bytes of 32 consecutive elements of a weight row, in the low bytes: 4, 2 or 1 of them (SB = 8, 16, 32 and more).
+// Four scale bytes (SB = 8: those of 32 elements), or one in the low byte.
 template <int SB>
 __device__ __forceinline__ uint32_t buffer_load_scales(__amdgpu_buffer_rsrc_t b, uint32_t at, int scalar)
 {
     if constexpr (SB == 8) return __builtin_amdgcn_raw_buffer_load_b32(b, (int)at, scalar, 0);
-    else if constexpr (SB == 16) return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, (int)at, scalar, 0);
     else return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(b, (int)at, scalar, 0);
 }
 
@@ -868,14 +867,22 @@ hipError_t launch_products(const LinearArgs& a, const LinearPlan& p, hipStream_t
         // Wavefronts beside each other in n where elements are widened, so that no code is widened twice (256 x 256: 831 -> 796 us at 4096 x
         // 28672 x 4096); in two rows where they multiply as they are, which reads less of LDS.
         constexpr bool kWide = XT != kXMx;
+        if constexpr (!kWide)
+            if (p.mt == 8) {
+                launch_tiled<XT, SB, 4, 2, 4, 4, 3>(a, p, stream);
+                return hipGetLastError();
+            }
         if (p.mt == 16) launch_tiled<XT, SB, kWide ? 8 : 4, kWide ? 1 : 2, kWide ? 2 : 4, kWide ? 16 : 8, 2>(a, p, stream);
-        else if (p.mt == 8) launch_tiled<XT, SB, kWide ? 8 : 4, kWide ? 1 : 2, kWide ? 2 : 4, kWide ? 8 : 4, XT == kXQ8 ? 2 : 3>(a, p, stream);
         else if (p.nt == 16) launch_tiled<XT, SB, kWide ? 8 : 4, kWide ? 1 : 2, kWide ? 2 : 4, kWide ? 4 : 2, kWide ? 2 : 4>(a, p, stream);
         else launch_tiled<XT, SB, kWide ? 8 : 4, kWide ? 1 : 2, kWide ? 1 : 2, kWide ? 4 : 2, kWide ? 2 : 4>(a, p, stream);
     } else {
         // one chunk ahead; two where it is 16 rows (4096 x 14336, one token: 11.6 -> 10.8 us; four 11.6; 64 rows, two 14.1, one 13.9)
-        if (p.mt == 2) launch_direct<XT, SB, 4, 2, 1>(a, p, stream);
-        else if (p.nt == 4) launch_direct<XT, SB, 4, 1, 1>(a, p, stream);
+        if constexpr (XT != kXBf16)                            // bf16 of more than 16 tokens goes to tiles
+            if (p.mt == 2) {
+                launch_direct<XT, SB, 4, 2, 1>(a, p, stream);
+                return hipGetLastError();
+            }
+        if (p.nt == 4) launch_direct<XT, SB, 4, 1, 1>(a, p, stream);
         else if (p.nt == 2) launch_direct<XT, SB, 2, 1, 1>(a, p, stream);
         else launch_direct<XT, SB, 1, 1, 2>(a, p, stream);
     }

@@ -47,22 +47,27 @@ struct LinearTile {
     int nt, mt;
     float alone, beside;
 };
-constexpr LinearTile kWidened[4] = {{16, 16, 3.6f, 3.6f}, {16, 8, 2.3f, 2.3f}, {16, 4, 1.4f, 1.13f}, {8, 4, 0.87f, 0.75f}};
+// Widened, 256 x 128 takes 2.3 us, more than two of 256 x 64: there is no such kernel.
+constexpr LinearTile kWidened[3] = {{16, 16, 3.6f, 3.6f}, {16, 4, 1.4f, 1.13f}, {8, 4, 0.87f, 0.75f}};
 constexpr LinearTile kScaled[4] = {{16, 16, 2.0f, 2.0f}, {16, 8, 1.1f, 1.1f}, {16, 4, 0.8f, 0.7f}, {8, 4, 0.55f, 0.42f}};
 
 inline LinearPlan plan_linear(const LinearShape& a)
 {
     LinearPlan p = {};
     const int chunks = (a.k + 127) / 128;
-    // 24 tokens, 14336 x 4096 bf16: direct 26 us, tiles 20; 4096 x 14336 scaled: 16 and 19
-    p.tiled = a.m > (a.scaled ? 32 : 16);
+    // 24 tokens, 14336 x 4096 bf16: direct 26 us, tiles 20; 4096 x 14336 scaled: 16 and 19.  Q8 that is widened, as long as 64 rows of W a
+    // workgroup make one round on the units (E8M0 block 32, direct and tiles): 4096 x 14336 17.4 and 26.2, 14336 x 4096 15.8 and 19.9, 1024 x 1024
+    // 6.4 and 10.3; beyond, 28672 x 4096: 30.2 and 28.1.
+    p.tiled = a.m > (a.scaled || (!a.bf16 && a.n <= 64 * kUnits) ? 32 : 16);
     int64_t groups = 1;
     int most = 1, fit = chunks;                            // parts of k at most, chunks in one at most
     int64_t splits = 1;
     if (p.tiled) {
         // The cut that takes least: rounds of workgroups on the units, and for more than one part of k the sums that are written and read.
         float least = 0.0f;
-        for (const LinearTile& t : a.scaled ? kScaled : kWidened) {
+        const LinearTile* const tile = a.scaled ? kScaled : kWidened;
+        for (int i = 0; i < (a.scaled ? 4 : 3); ++i) {
+            const LinearTile& t = tile[i];
             const int64_t tiles = (int64_t)((a.n + 16 * t.nt - 1) / (16 * t.nt)) * ((a.m + 16 * t.mt - 1) / (16 * t.mt));
             for (int s = 1; s <= 8 && (s == 1 || 4 * s <= chunks); ++s) {
                 const int64_t rounds = (tiles * s + kUnits - 1) / kUnits;
