@@ -117,11 +117,10 @@ MXQ_API int mxq_swiglu_backward(const void* dh, int64_t ld_dh, const uint8_t* ga
  *     y[i, :] = T * X[i, :] * W^T  +  scaling[a] * (X[i, :] * A[a]^T) * B[a]^T,   a = ids[i],
  * X the activations (m x k, bf16 or Q8), W[j, l] = q * S the packed weights (n x k), T their
  * per-tensor scale.  W is never unpacked in memory.  Products of elements are exact (bf16 holds q * S and
- * Q8's elements), sums are fp32, y is rounded once; the adapters' inner product enters the second one as
- * two bf16 parts (16 bits).  With MXQ_SUMS_MX, Q8 against E8M0 weights of block 32 and more, with a bf16
- * output, multiplies in the formats themselves, up to twice as fast: the scaled matrix instruction sums 128
- * products with an error of up to 2^-14 of their magnitudes (2^-18 where their sizes are alike) before it
- * adds them in fp32.
+ * Q8's elements), sums are fp32, the adapters' inner product among them, y is rounded once.  With
+ * MXQ_SUMS_MX, Q8 against E8M0 weights of block 32 and more, with a bf16 output, multiplies in the formats
+ * themselves, up to twice as fast: the scaled matrix instruction sums 128 products with an error of up to
+ * 2^-14 of their magnitudes (2^-18 where their sizes are alike) before it adds them in fp32.
  *
  *   x, ld_x       device, m x k bf16, rows 16-byte aligned; NULL if x_codes is given
  *   x_codes, x_scales   device, m x k as Q8, 16-byte and 1-byte aligned; NULL if x is given

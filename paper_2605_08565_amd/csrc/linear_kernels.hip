@@ -106,9 +106,18 @@ __device__ __forceinline__ void store_y(const LinearArgs& a, int m, int n, f32x4
     }
 }
 
+// The top halves of 8 values: bf16 that is cut off.
+__device__ __forceinline__ uint4 cut_of8(const float (&v)[8])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = f2u(v[2 * i]) >> 16 | (f2u(v[2 * i + 1]) & 0xFFFF0000u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Adds B_a * low^T to NT tiles, side by side, of the same 16 tokens: one adapter after the other, each kept by its tokens alone (not
-// added as zeros to the others, where an infinity in B would be NaN).  `low` (fp32) enters as a high and a low bf16 part, which
-// keeps 16 of its bits.
+// added as zeros to the others, where an infinity in B would be NaN).  `low` (fp32) enters as three bf16 parts of 8 bits, cut off and
+// not rounded: all of its 24 bits, and none of them beyond bf16's range.
 template <int NT>
 __device__ __forceinline__ void add_adapters(const LinearArgs& a, int m, int n0, f32x4 (&acc)[NT])
 {
@@ -123,7 +132,7 @@ __device__ __forceinline__ void add_adapters(const LinearArgs& a, int m, int n0,
         for (int i = 0; i < NT; ++i) sum[i] = acc[i];
         for (int r0 = 0; r0 < a.rank; r0 += 32) {
             const int r = r0 + 8 * g;
-            float u[8] = {}, rest[8];
+            float u[8] = {}, mid[8], rest[8];
             if (r < a.rank && mine) {
                 load8<kF32>(a.low, (int64_t)m * a.rank + r, u);
                 for (int p = 1; p < a.low_parts; ++p) {
@@ -133,17 +142,18 @@ __device__ __forceinline__ void add_adapters(const LinearArgs& a, int m, int n0,
                     for (int i = 0; i < 8; ++i) u[i] += more[i];
                 }
             }
-            const uint4 hi = bf16_of8(u);
-            const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] = u[i] - u2f((i & 1) ? (h[i / 2] & 0xFFFF0000u) : (h[i / 2] << 16));
-            const uint4 lo = bf16_of8(rest);
+            for (int i = 0; i < 8; ++i) {
+                mid[i] = u[i] - u2f(f2u(u[i]) & 0xFFFF0000u);
+                rest[i] = mid[i] - u2f(f2u(mid[i]) & 0xFFFF0000u);
+            }
+            const uint4 parts[3] = {cut_of8(rest), cut_of8(mid), cut_of8(u)};          // the small ones first
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
                 if (r < a.rank) w = *reinterpret_cast<const uint4*>(a.b + ((int64_t)cur * a.n + min(n0 + 16 * i + (lane & 15), a.n - 1)) * a.rank + r);
-                sum[i] = mfma_bf16(w, lo, sum[i]);
-                sum[i] = mfma_bf16(w, hi, sum[i]);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) sum[i] = mfma_bf16(w, parts[p], sum[i]);
             }
         }
 #pragma unroll
