@@ -115,9 +115,22 @@ __device__ __forceinline__ uint4 cut_of8(const float (&v)[8])
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// 8 bf16 values with zeros in place of infinities and NaN.
+__device__ __forceinline__ uint4 finite_of8(uint4 v)
+{
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x00007F80u) == 0x00007F80u) w[i] &= 0xFFFF0000u;
+        if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0x0000FFFFu;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Adds B_a * low^T to NT tiles, side by side, of the same 16 tokens: one adapter after the other, each kept by its tokens alone (not
 // added as zeros to the others, where an infinity in B would be NaN).  `low` (fp32) enters as three bf16 parts of 8 bits, cut off and
-// not rounded: all of its 24 bits, and none of them beyond bf16's range.
+// not rounded: all of its 24 bits, and none of them beyond bf16's range.  Infinities of `low` and of B meet the first part alone, which has
+// the sign of the whole: the others would be infinity - infinity, or 0 * infinity.
 template <int NT>
 __device__ __forceinline__ void add_adapters(const LinearArgs& a, int m, int n0, f32x4 (&acc)[NT])
 {
@@ -144,16 +157,18 @@ __device__ __forceinline__ void add_adapters(const LinearArgs& a, int m, int n0,
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                mid[i] = u[i] - u2f(f2u(u[i]) & 0xFFFF0000u);
+                mid[i] = __builtin_isfinite(u[i]) ? u[i] - u2f(f2u(u[i]) & 0xFFFF0000u) : 0.0f;
                 rest[i] = mid[i] - u2f(f2u(mid[i]) & 0xFFFF0000u);
             }
-            const uint4 parts[3] = {cut_of8(rest), cut_of8(mid), cut_of8(u)};          // the small ones first
+            const uint4 first = cut_of8(u), second = cut_of8(mid), third = cut_of8(rest);
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
                 if (r < a.rank) w = *reinterpret_cast<const uint4*>(a.b + ((int64_t)cur * a.n + min(n0 + 16 * i + (lane & 15), a.n - 1)) * a.rank + r);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) sum[i] = mfma_bf16(w, parts[p], sum[i]);
+                const uint4 finite = finite_of8(w);
+                sum[i] = mfma_bf16(finite, third, sum[i]);             // the small ones first
+                sum[i] = mfma_bf16(finite, second, sum[i]);
+                sum[i] = mfma_bf16(w, first, sum[i]);
             }
         }
 #pragma unroll
