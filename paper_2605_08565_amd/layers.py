@@ -2,7 +2,9 @@
 
 As in mxq.py: argument marshalling only, on tensors that live on the GPU, enqueued on the current stream; nothing is
 computed here and there is no CPU fallback.  Gradients are calls of their own (the operators do not record for
-autograd; mlp.py wraps them).  Tensors made by a call are allocated on the current stream.
+autograd; mlp.py wraps them).  Tensors made by a call are allocated on the current stream, workspaces on the stream
+that the call is enqueued on.  As for any tensor of torch, a caller who passes another stream makes it wait for the
+current one before the call and records it on the outputs after.
 
 As there, each call has a native form (csrc/layers_binding.cpp, built as _mxq_layer_calls.so) that is asked first and
 declines, before it has done anything, whatever is not plain; the Python form below is the definition of the call.
@@ -155,11 +157,12 @@ def _check_q8(q: Q8, name: str, shape, device) -> None:
 
 
 def _workspace(nbytes: int, device, stream) -> torch.Tensor:
-    """Scratch memory of one call: allocated on the current stream, and kept until `stream` is through with it."""
-    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+    """Scratch memory of one call, allocated on the stream that uses it: memory that was freed on the current stream may still be
+    written there, and the caller, who does not see the workspace, could not make `stream` wait for that."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def _ptr(t):
