@@ -15,6 +15,7 @@ import json
 import time
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import layers, mxq
 from .layers import Adapters, Q8, SavedNorm, SavedSwiglu, W4
@@ -60,6 +61,7 @@ class AddRMSNorm(torch.autograd.Function):
         return y, hidden
 
     @staticmethod
+    @once_differentiable                                  # the kernels record nothing: second derivatives are an error, not zero
     def backward(ctx, dy, dhidden):
         weight, codes, scales, rstd = ctx.saved_tensors
         if dy is None:
@@ -80,6 +82,7 @@ class SwiGLU(torch.autograd.Function):
         return h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         gc, gs, uc, us = ctx.saved_tensors
         dgate, _, _ = layers.swiglu_backward(dh.contiguous(), SavedSwiglu(Q8(gc, gs), Q8(uc, us)))
