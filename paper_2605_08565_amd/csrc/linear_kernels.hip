@@ -257,11 +257,12 @@ __global__ void __launch_bounds__(64 * kWaves) lowrank_kernel(LinearArgs a)
 }
 
 // 16 bytes a lane from a buffer to LDS, lane l to `lds` + 16 l, no registers in between; zeros for an offset beyond the buffer.  Not
-// counted by the compiler: the caller waits with all_loads_done().  (The compiler gives m0 to nothing in between two instructions.)
+// counted by the compiler: the caller waits with all_loads_done().  m0, which holds the place in LDS, is an operand: the compiler writes it
+// and knows that it has (one wait state has to lie between that and the load).
 using i32x4 = int __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t at, int scalar, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(buffer), "s"(scalar) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds), "v"(at), "s"(buffer), "s"(scalar) : "memory");
 }
 // The four words of a descriptor as buffer_of() makes it: address, no stride, size, format.
 __device__ __forceinline__ i32x4 buffer_words(const void* base, uint32_t bytes)
