@@ -967,8 +967,7 @@ hipError_t launch_rows(LinearArgs a, void* workspace, hipStream_t stream)
     return e;
 }
 
-// Rows of one launch: a grid's second side is short, and a tile's rows of x span less than 4 GiB (32-bit offsets), or go one by one.
-int64_t rows_a_launch(const LinearArgs& a) { return a.x && a.ld_x >= (1 << 22) ? 1 : (int64_t)1 << 19; }
+int64_t rows_a_launch(const LinearArgs& a) { return a.x ? linear_rows_a_launch(a.m, a.ld_x) : kMostRows; }
 
 }  // namespace
 

@@ -26,6 +26,17 @@ struct LinearPlan {
     size_t low_bytes, part_bytes;                          // of the workspace
 };
 
+// Rows of one launch over bf16 rows ld elements apart: a grid's second side is short, and the rows of a workgroup span at most 2 GiB (32-bit
+// offsets).  256 rows of a tile do so below a stride of 2^22, the 16 of the direct kernel below 2^26 (the last tokens of prompts of
+// 1024 x 4096 and more; 16 of them by 14336 x 4096 one by one 158 us, together 14.6).  Beyond, rows go one by one.
+constexpr int64_t kMostRows = (int64_t)1 << 19;
+
+inline int64_t linear_rows_a_launch(int64_t m, int64_t ld)
+{
+    if (m <= 1 || ld < (int64_t)1 << 22) return kMostRows;
+    return ld < (int64_t)1 << 26 ? 16 : 1;
+}
+
 // LDS of a workgroup of the direct kernel: tokens first, which the sums of its wavefronts replace later.
 struct DirectLds { int x_scales, w_scales, bytes; };
 
