@@ -125,9 +125,10 @@ struct Raw8 {
 
 // A group of TPR threads goes over rows g, g + groups, ... and keeps its part of the weight's gradient in registers; what is
 // left at the end is one row of partial sums per group, added up by norm_weight_kernel in the groups' order.  Bound by memory: the
-// next row is loaded, as it is, while this one is summed (behind the last one: the last row again, for nothing).  8192 x 4096 bf16 with
-// dhidden (236 MB and 8 MB of partial sums) 78 -> 41 us by that, 5.9 TB/s; 512 groups (two workgroups a unit) against 256, 384, 768 and 1024:
-// 44.8 us with the second launch, 51.1, 52.8, 48.2, 52.4.
+// next row is loaded, as it is, while this one is summed (behind its last one a group loads that one again, for nothing: never a row
+// that another group may be writing, where dx is dy or dhidden itself).  8192 x 4096 bf16 with dhidden (236 MB and 8 MB of partial sums)
+// 78 -> 41 us by that, 5.9 TB/s; 512 groups (two workgroups a unit) against 256, 384, 768 and 1024: 44.8 us with the second launch,
+// 51.1, 52.8, 48.2, 52.4.
 template <int DT, int TPR, int CH>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) add_rmsnorm_backward_kernel(NormBackArgs a, int64_t groups)
 {
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) add_rmsnorm_backward_ke
     Row now = {}, next = {};
     load(group, now);
     for (int64_t row = group; row < a.rows; row += groups, parity ^= 1) {
-        load(row + groups < a.rows ? row + groups : a.rows - 1, next);
+        load(row + groups < a.rows ? row + groups : row, next);
         float g[CH][8], n[CH][8];
         float along = 0.0f;
 #pragma unroll
