@@ -106,6 +106,12 @@ struct Raw8 {
         v[0] = q[0];
         if constexpr (DT != kBF16) v[1] = q[1];
     }
+    // What was made of it has to be made again.
+    __device__ void forget()
+    {
+        asm volatile("" : "+v"(v[0].x), "+v"(v[0].y), "+v"(v[0].z), "+v"(v[0].w));
+        if constexpr (DT != kBF16) asm volatile("" : "+v"(v[1].x), "+v"(v[1].y), "+v"(v[1].z), "+v"(v[1].w));
+    }
     __device__ void widen(float (&f)[8]) const
     {
         const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
@@ -127,18 +133,25 @@ struct Raw8 {
 // left at the end is one row of partial sums per group, added up by norm_weight_kernel in the groups' order.  Bound by memory: the
 // next row is loaded, as it is, while this one is summed (behind its last one a group loads that one again, for nothing: never a row
 // that another group may be writing, where dx is dy or dhidden itself).  8192 x 4096 bf16 with dhidden (236 MB and 8 MB of partial sums)
-// 78 -> 41 us by that, 5.9 TB/s; 512 groups (two workgroups a unit) against 256, 384, 768 and 1024: 44.8 us with the second launch,
-// 51.1, 52.8, 48.2, 52.4.
+// 78 -> 41 us by that, 5.9 TB/s; 512 groups against 256, 384, 768 and 1024: 44.8 us with the second launch, 51.1, 52.8, 48.2, 52.4.
+//
+// Rows of 1024 threads are tight: a thread has 128 registers, and two rows with the weight and its gradient do not fit (they spilled
+// 25 registers in bf16 and 101 in fp32).  There the weight and its gradient are in LDS, a place for each thread, dhidden is loaded with
+// its row and not ahead of it, and what was widened for the sum is widened once more for dx.  With the second launch, 2048 x 16384 with
+// dhidden 120 -> 66 us in bf16 and 321 -> 119 in fp32, 2048 x 8224 74 -> 37 and 147 -> 46.
 template <int DT, int TPR, int CH>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) add_rmsnorm_backward_kernel(NormBackArgs a, int64_t groups)
 {
     constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
+    constexpr bool kTight = TPR == 1024;
     __shared__ float slots[2][16];
+    __shared__ Raw8<DT> weights[kTight ? CH : 1][kTight ? TPR : 1];        // tight: a thread's part of the weight, and of its gradient
+    __shared__ f32x4 dw_parts[kTight ? 2 * CH : 1][kTight ? TPR : 1];
     const int lane = threadIdx.x % TPR;
     const int64_t group = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
     if (group >= groups) return;
     struct Row {
-        Raw8<DT> dy[CH], dh[CH];
+        Raw8<DT> dy[CH], dh[kTight ? 1 : CH];
         uint2 n[CH];
         uint32_t scale[CH];
         float rstd;
@@ -152,53 +165,85 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) add_rmsnorm_backward_ke
                 r.dy[k].load(a.dy, row * a.ld_dy + c);
                 r.n[k] = *reinterpret_cast<const uint2*>(a.n_codes + at);
                 r.scale[k] = a.n_scales[at >> 5];
-                if (a.dhidden) r.dh[k].load(a.dhidden, row * a.ld_dhidden + c);
+                if constexpr (!kTight)
+                    if (a.dhidden) r.dh[k].load(a.dhidden, row * a.ld_dhidden + c);
             }
         }
         r.rstd = a.rstd[row];
     };
-    Raw8<DT> weight[CH];
+    Raw8<DT> weight[kTight ? 1 : CH];
 #pragma unroll
     for (int k = 0; k < CH; ++k)
-        if (a.weight && (k * TPR + lane) * 8 < a.cols) weight[k].load(a.weight, (k * TPR + lane) * 8);
+        if (a.weight && (k * TPR + lane) * 8 < a.cols) {
+            if constexpr (kTight) weights[k][lane].load(a.weight, (k * TPR + lane) * 8);
+            else weight[k].load(a.weight, (k * TPR + lane) * 8);
+        }
     float dw[CH][8] = {};
+    if constexpr (kTight) {
+#pragma unroll
+        for (int j = 0; j < 2 * CH; ++j) dw_parts[j][lane] = f32x4{};
+    }
     int parity = 0;
     Row now = {}, next = {};
     load(group, now);
     for (int64_t row = group; row < a.rows; row += groups, parity ^= 1) {
+        Raw8<DT> dh[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if constexpr (!kTight) dh[k] = now.dh[k];
+            else if (a.dhidden && (k * TPR + lane) * 8 < a.cols) dh[k].load(a.dhidden, row * a.ld_dhidden + (k * TPR + lane) * 8);
+        }
         load(row + groups < a.rows ? row + groups : row, next);
-        float g[CH][8], n[CH][8];
+        // dy and n of a chunk, zeros behind the row's end; and g in the place of dy.
+        auto widen = [&](int k, float (&d)[8], float (&n)[8]) {
+            const bool in = (k * TPR + lane) * 8 < a.cols;
+            now.dy[k].widen(d);
+            q8_widen(now.n[k], q8_scale(now.scale[k]), n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!in) d[i] = n[i] = 0.0f;
+        };
+        auto weigh = [&](int k, float (&d)[8]) {
+            if (!a.weight) return;
+            const bool in = (k * TPR + lane) * 8 < a.cols;
+            float w[8];
+            if constexpr (kTight) weights[k][lane].widen(w);
+            else weight[k].widen(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = in ? d[i] * w[i] : 0.0f;
+        };
+        float g[kTight ? 1 : CH][8], n[kTight ? 1 : CH][8];
         float along = 0.0f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const bool in = (k * TPR + lane) * 8 < a.cols;
-            now.dy[k].widen(g[k]);
-            q8_widen(now.n[k], q8_scale(now.scale[k]), n[k]);
+            const int at = kTight ? 0 : k;
+            widen(k, g[at], n[at]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (!in) g[k][i] = n[k][i] = 0.0f;
-                dw[k][i] += g[k][i] * n[k][i];
+                if constexpr (kTight) dw_parts[2 * k + i / 4][lane][i % 4] += g[at][i] * n[at][i];
+                else dw[k][i] += g[at][i] * n[at][i];
             }
-            if (a.weight) {
-                float w[8];
-                weight[k].widen(w);
+            weigh(k, g[at]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[k][i] = in ? g[k][i] * w[i] : 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) along += g[k][i] * n[k][i];
+            for (int i = 0; i < 8; ++i) along += g[at][i] * n[at][i];
         }
         along = row_sum<TPR>(along, slots[parity]) / (float)a.cols;       // the other slots may still be read: two in turn
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * TPR + lane) * 8;
+            const int c = (k * TPR + lane) * 8, at = kTight ? 0 : k;
             if (c >= a.cols) continue;
+            if constexpr (kTight) {
+                now.dy[k].forget();                         // or the compiler keeps what was widened
+                asm volatile("" : "+v"(now.n[k].x), "+v"(now.n[k].y));
+                widen(k, g[0], n[0]);
+                weigh(k, g[0]);
+            }
             float dx[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dx[i] = now.rstd * (g[k][i] - n[k][i] * along);
+            for (int i = 0; i < 8; ++i) dx[i] = now.rstd * (g[at][i] - n[at][i] * along);
             if (a.dhidden) {
                 float d[8];
-                now.dh[k].widen(d);
+                dh[k].widen(d);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dx[i] += d[i];
             }
@@ -210,6 +255,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) add_rmsnorm_backward_ke
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int c = (k * TPR + lane) * 8;
+        if constexpr (kTight) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dw[k][i] = dw_parts[2 * k + i / 4][lane][i % 4];
+        }
         if (c < a.cols) store8<kF32>(a.partial, group * a.cols + c, dw[k]);
     }
 }
