@@ -302,9 +302,10 @@ __device__ __forceinline__ uint32_t piece_of(uint32_t row, uint32_t piece)
 // What bounds it: the bytes of W.  Reading 14336 x 2048 bytes of codes 16 rows at a time takes 6.2 us and is as fast as reading them
 // in a line (5.9).  A lane needs 1 to 4 scale bytes of each row for a chunk: loaded by the lanes that need them they cost 3.5 us of 12.1
 // (7 of 20.2 with 28672 rows), because every such load touches 16 lines for a few bytes of each; they come to LDS in whole lines
-// instead, once a workgroup, and so do the activations, which every wavefront would load again.  One token, 14336 x 4096 E4M3 (33 MB) 11 us,
-// 28672 x 4096 in 8 bits (62 MB) 12.7 us, 4.9 TB/s; 24 tokens x 4096 x 14336 in 8 bits 11.8 us.  The widening, two instructions a weight, is 3.9 us of the
-// first if nothing hides it: small workgroups, so that some load while others multiply.
+// instead, once a workgroup, and so do the activations, which every wavefront would load again.  One token, 14336 x 4096 E4M3 (33 MB)
+// 10.7 us; Q8 against E8M0, one token, 28672 x 4096 (62 MB) 23.1 us, by the scaled instruction 15.7; 24 tokens x 4096 x 14336 15.1 and
+// 11.3.  The widening, two instructions a weight, is 3.9 us of the first if nothing hides it: small workgroups, so that some load while
+// others multiply.
 // ---------------------------------------------------------------------------------------
 template <int XT, int SB, int NT, int MT, int AHEAD>
 __global__ void __launch_bounds__(64 * kWaves) linear_direct_kernel(LinearArgs a, int main_blocks, DirectLds lds)
@@ -491,9 +492,9 @@ __global__ void __launch_bounds__(64 * kWaves) linear_direct_kernel(LinearArgs a
     }
 }
 
-// Adds up the parts of k of a few tokens, and their adapters, each lane for its token: every load of the lane stands on its own, however
-// many different adapters the tokens have (24 tokens with 12 adapters: one adapter after the other 12.7 us, so 6.3; 4.0 without).  A wavefront
-// has one tile.
+// Adds up the parts of k of a few tokens, and their adapters, each lane for its token, however many different adapters the tokens have (24
+// tokens with 12 adapters, 7 parts: one adapter after the other 12.7 us, so 6.0; 3.9 without).  A wavefront has one tile.  Bound by its
+// trips to memory, one behind the other: a part of k, then the next, then the parts of the inner product.
 __global__ void __launch_bounds__(256) linear_join_few_kernel(LinearArgs a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -527,7 +528,7 @@ __global__ void __launch_bounds__(256) linear_join_few_kernel(LinearArgs a)
 }
 
 // Adds up the parts of k, and the adapters.  A wavefront has 16 tokens and NT tiles of 16 columns.  Bound by memory: two parts of 2048 x
-// 4096 (67 MB in, 17 out) 17 us, with 8 adapters 22.
+// 4096 (67 MB in, 17 out) 15.8 us, with 8 adapters in order 23.4, mixed (6.5 to a tile) 49.5.
 template <int NT>
 __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a)
 {
@@ -549,13 +550,13 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a)
 }
 
 // ---------------------------------------------------------------------------------------
-// Many tokens: tiles of BN rows of W times BM tokens, eight wavefronts, k in chunks of 128.  The activations go through LDS
-// (two chunks in turn, the next one on its way while this one is multiplied); the weights, a quarter of their size or less, go from
-// memory to the registers of the wavefronts that multiply them and are widened there, so LDS neither holds nor moves them.
-// LDS rows are 256 bytes (bf16) or 128 (Q8 as it is) without padding; 16-byte pieces of a row are permuted by the row number, so
+// Many tokens: tiles of BN rows of W times BM tokens, eight wavefronts, k in chunks of 128.  Tokens, codes and scales all go through LDS,
+// straight from memory but for Q8 that is widened (its tokens pass through registers, where they become bf16).  LDS has STAGES chunks in
+// turn; the codes have one buffer where it has no room for more.  Codes are widened behind LDS, by the wavefronts that multiply them.
+// LDS rows of tokens are 256 bytes (bf16) or 128 (Q8 as it is) without padding; 16-byte pieces of a row are permuted by the row number, so
 // that the 16 rows of a fragment read 16 (8) different groups of banks.
-// What bounds it: the matrix instructions, with the loads and the widening not quite behind them.  4096 x 28672 x 4096: 8 bits 417 us (2.3
-// PFLOP/s; 311 with all loads taken out), bf16 against E4M3 790 (1.2; 515).  A lane's own loads of scale bytes cost 180 us of the first when it had them.
+// What bounds it: the matrix instructions, with the loads and the widening not quite behind them.  4096 x 28672 x 4096, the kernel alone:
+// Q8 against E8M0 by the scaled instruction 409 us (2.35 PFLOP/s), widened 960 (1.0); bf16 against E4M3 776 (1.24).
 // ---------------------------------------------------------------------------------------
 constexpr int kTiledThreads = 512;
 

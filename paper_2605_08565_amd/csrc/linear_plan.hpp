@@ -51,7 +51,8 @@ inline DirectLds direct_lds(const LinearShape& a, int nt, int mt, int chunks_eac
     return l;
 }
 
-// Tiles of the tiled kernel, and what a chunk of 128 of one takes on a unit, in us: alone there, and beside others.  Measured at
+// Tiles of the tiled kernel, and what a chunk of 128 of one takes on a unit, in us: alone there, and beside others (for bf16; widened Q8
+// takes a quarter more in each and goes by the same table).  Measured at
 // 4096 x 28672 x 4096, 512 x 14336 x 4096, 128 x 14336 x 4096 and 64 x 14336 x 4096 (bf16 against E4M3) and 4096 x 28672 x 4096 and 512 x 4096 x 4096
 // (scaled).
 struct LinearTile {
@@ -66,7 +67,7 @@ inline LinearPlan plan_linear(const LinearShape& a)
 {
     LinearPlan p = {};
     const int chunks = (a.k + 127) / 128;
-    // 24 tokens, 14336 x 4096 bf16: direct 26 us, tiles 20; 4096 x 14336 scaled: 16 and 19.  Q8 that is widened, as long as 64 rows of W a
+    // 24 tokens, 14336 x 4096 bf16: direct 26 us, tiles 18; 4096 x 14336 scaled: 12.9 and 16.4.  Q8 that is widened, as long as 64 rows of W a
     // workgroup make one round on the units (E8M0 block 32, direct and tiles): 4096 x 14336 17.4 and 26.2, 14336 x 4096 15.8 and 19.9, 1024 x 1024
     // 6.4 and 10.3; beyond, 28672 x 4096: 30.2 and 28.1.
     p.tiled = a.m > (a.scaled || (!a.bf16 && a.n <= 64 * kUnits) ? 32 : 16);
@@ -106,8 +107,8 @@ inline LinearPlan plan_linear(const LinearShape& a)
         most = chunks / kLinearWaves;
     }
     if (!p.tiled) {
-        // one workgroup a unit; with the adapters' workgroups beside them nearly two (24 x 4096 x 14336, 12 adapters: 4 parts 23.2 us, 7 21.6, 10
-        // 22.5).  Adapters behind a product of their own, without the last launch: 16 x 14336 x 4096 18.5 us against 14.2.
+        // one workgroup a unit; with the adapters' workgroups beside them nearly two (24 x 4096 x 14336, 12 adapters, scaled: 4 parts 23.2 us,
+        // 7 21.6, 10 22.5; one size, and a kernel of which two lie on a unit: of widened Q8 for more than 16 tokens one does, 30.5 and 32.3).  Adapters behind a product of their own, without the last launch: 16 x 14336 x 4096 18.5 us against 14.2.
         const int64_t want = (a.rank > 0 ? kUnits * 7 / 4 : kUnits) / groups;
         splits = want < most ? want : most;
         if (splits < 1) splits = 1;

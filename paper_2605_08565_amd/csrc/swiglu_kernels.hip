@@ -26,7 +26,7 @@ struct Place {
 };
 
 // One lane has 8 consecutive elements; blocks of 32 are quads of lanes, and all of a quad is inside or none.  No loop and no LDS: bound
-// by memory.  4096 x 14336 bf16, dense output and checkpoint (473 MB) 85 us, 5.6 TB/s; 16 rows 2.6 us.
+// by memory.  4096 x 14336 bf16, dense output and checkpoint (473 MB) 87 us, 5.4 TB/s; 16 rows 2.8 us.
 template <int DT>
 __global__ void __launch_bounds__(256) swiglu_kernel(SwigluArgs a)
 {
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) swiglu_kernel(SwigluArgs a)
     }
 }
 
-// 4096 x 14336 bf16 with the output again (591 MB) 114 us, 5.2 TB/s.
+// 4096 x 14336 bf16 with the output again (591 MB) 111 to 115 us, 5.2 TB/s.
 template <int DT>
 __global__ void __launch_bounds__(256) swiglu_backward_kernel(SwigluBackArgs a)
 {

@@ -72,7 +72,8 @@ class AddRMSNorm(torch.autograd.Function):
 
 
 class SwiGLU(torch.autograd.Function):
-    """h = apply(both): gate and up are the halves of [tokens, 2 * width], kept in 8 bits."""
+    """h = apply(both): gate and up are the halves of [tokens, 2 * width], kept in 8 bits.  h itself stays with the product behind it, whose
+    weight gradient is then that of the h it multiplied; swiglu_backward(again=True) forms h from the 8 bits for who would rather not keep it."""
 
     @staticmethod
     def forward(ctx, both):
